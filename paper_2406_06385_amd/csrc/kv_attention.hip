@@ -58,6 +58,12 @@ __device__ __forceinline__ float sane(float s) { return s < kKvMinScale ? kKvMin
 
 constexpr float kNone = -__builtin_inff();
 constexpr float kBias = 14.f;  // the largest weight is 2^14
+// What the exponents are taken from, given the largest one: kBias below it.  From 2^25 on float32 may put that 16 below,
+// and half precision ends short of 2^16; so there, where an exponent is a multiple of 4 anyway, without the bias.
+__device__ __forceinline__ float below(float mx) {
+  const float m = mx - kBias;
+  return mx - m <= kBias + 1.f ? m : mx;  // (mx where it is an infinity)
+}
 
 // What a block works on.
 struct Tile {
@@ -213,7 +219,7 @@ __global__ __launch_bounds__(64 * NW, DH == 4 ? 1 : 2) void k_kv_attn_rows(KvAtt
       mx = fmaxf(mx, w[j]);
     }
     mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32)) - kBias;
+    mx = below(fmaxf(mx, __shfl_xor(mx, 32)));
     const float m1 = fmaxf(m, mx), mf = m1 == kNone ? 0.f : m1;
     const float alpha = exp2_(m - mf);
     m = m1;
@@ -517,10 +523,10 @@ __global__ __launch_bounds__(64 * NW, DP == 256 ? 1 : 2) void k_kv_attn_many(KvA
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int j = 0; j < 16; ++j) mx = fmaxf(mx, s[t][j]);
-    // The maximum follows only from twice the weight on (weights stay below 2^15): few steps pay for it, or for the
-    // exchange between the two lanes of a row.
-    if (__any(mx > m + (kBias + 1.f))) {
-      const float m1 = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32)) - kBias), alpha = exp2_(m - (m1 == kNone ? 0.f : m1));
+    // The maximum follows only from twice the weight on (weights stay within 2^15; the difference is exact where it is
+    // near that, a sum would be rounded): few steps pay for it, or for the exchange between the two lanes of a row.
+    if (__any(mx - m > kBias + 1.f)) {
+      const float m1 = fmaxf(m, below(fmaxf(mx, __shfl_xor(mx, 32)))), alpha = exp2_(m - (m1 == kNone ? 0.f : m1));
       m = m1;
       l *= alpha;
 #pragma unroll

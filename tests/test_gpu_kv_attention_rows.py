@@ -62,6 +62,46 @@ def test_against_float64(lr, key, causal):
 
 
 @pytest.mark.parametrize("key", SOME, ids=SOME_IDS)
+def test_scales_far_apart_and_peaked_scores(lr, key):
+    S = Setup(lr, *SHAPES[key], seed=52, spread=6.0)
+    S.check()
+    S = Setup(lr, *SHAPES[key], seed=53)
+    S.scale = 3.0
+    S.check()
+
+
+FEW = {"one token": (4, 2, 64, 64, 1, [1, 1], [300, 90]), "one token, split": (4, 1, 128, 64, 1, [1], [3000])}
+
+
+@pytest.mark.parametrize("key", list(FEW) + SOME, ids=list(FEW) + SOME_IDS)
+def test_scores_that_float32_holds_in_steps(lr, key):
+    """Scores of 2^20 to 2^60: what a row sees of the largest code has all the weight, in equal parts, and no weight
+    leaves half precision.  The scores of one code are the same float32, those of two are a 2^7-th apart at least; the
+    average is of exact values, rounded to bfloat16."""
+    S = Setup(lr, *(FEW[key] if key in FEW else SHAPES[key]), seed=59)
+    hot = 0
+    for t in (S.cache.k, S.cache.v_scale):
+        t.zero_()
+    S.cache.v_scale.fill_(1.0)
+    S.cache.k[..., hot] = torch.arange(S.page, device="cuda").remainder(100).to(torch.int8)
+    q = torch.zeros_like(S.q)
+    q[..., hot] = 1.0
+    ref = torch.empty(S.q.shape, dtype=torch.float64, device="cuda")
+    for i, (a, c) in enumerate(zip(S.new, S.cached)):
+        for h in range(S.hkv):
+            v = S.cache.v[torch.from_numpy(S.table[i, :-(-(a + c) // S.page)]).long().cuda(), h].double().reshape(-1, S.d)
+            code = torch.arange(len(v), device="cuda") % S.page % 100
+            for r in range(a):
+                best = code[:c + r + 1] == code[:c + r + 1].max()
+                group = S.hq // S.hkv
+                ref[int(S.first[i]) + r, h * group:(h + 1) * group] = v[:c + r + 1][best].mean(0)
+    for exponent in (20, 23, 24, 24.5, 25, 25.3, 26, 27.7, 28, 31, 40, 60):
+        S.cache.k_scale.fill_(2.0 ** exponent / 64)
+        O = lr.lrqat_kv_attention(S.cache, S.batch(), q, scale=1.0)
+        assert ((O.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -10 * 127).all(), exponent
+
+
+@pytest.mark.parametrize("key", SOME, ids=SOME_IDS)
 def test_scores_that_rise_and_fall_along_the_keys(lr, key):
     """Every row's largest score moves up by a little at a time, and down again: one step's maximum is within, at and
     past twice the weight of the one before."""
