@@ -126,7 +126,7 @@ __global__ __launch_bounds__(64 * NW, DH == 4 ? 1 : 2) void k_kv_attn_rows(KvAtt
   const uint32_t qi = uint32_t(rr) / uint32_t(a.group), head = tl.head * a.group + uint32_t(rr) % uint32_t(a.group);
   const int64_t token = tl.row0 + qi;
   const int limit = row_limit(a, tl, rr);
-  const int k0 = tl.split * a.chunk, k1 = min(k0 + a.chunk, row_limit(a, tl, min(tl.r0 + kRowTile, tl.rows) - 1) + 1);
+  const int k0 = tl.split * a.chunk, k1 = kv_split_end(tl.split, a.chunk, row_limit(a, tl, min(tl.r0 + kRowTile, tl.rows) - 1) + 1);
   if (k0 >= k1 && tl.split > 0) return;  // (split 0 of a sequence without keys writes its zeros)
 
   u32x4 qf[DH][2];
@@ -371,7 +371,7 @@ __global__ __launch_bounds__(64 * NW, DP == 256 ? 1 : 2) void k_kv_attn_many(KvA
   const int64_t token = tl.row0 + qi;
   const int limit = row_limit(a, tl, rr);
   const int wave_first = row_limit(a, tl, w0), wave_last = row_limit(a, tl, min(w0 + 31, max(tl.rows - 1, w0)));
-  const int k0 = tl.split * a.chunk, k1 = min(k0 + a.chunk, row_limit(a, tl, min(tl.r0 + 32 * NW, tl.rows) - 1) + 1);
+  const int k0 = tl.split * a.chunk, k1 = kv_split_end(tl.split, a.chunk, row_limit(a, tl, min(tl.r0 + 32 * NW, tl.rows) - 1) + 1);
   if (k0 >= k1 && tl.split > 0) return;
 
   u32x4 qf[DP / 16];

@@ -74,4 +74,10 @@ inline KvAttnPlan kv_attn_plan(const KvSizes& z) {
   return p;
 }
 
+// The keys of a split among the first `seen`: from split * chunk up to here (at or below that: none).  The sum is formed
+// only where it is a key, as the splits of 2^31 - 2^16 positions may end past 2^31.
+constexpr int kv_split_end(int split, int chunk, int seen) {
+  return seen - split * chunk > chunk ? split * chunk + chunk : seen;
+}
+
 }  // namespace lrqat
