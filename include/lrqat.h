@@ -343,7 +343,9 @@ typedef struct {
   const int32_t* cached;      /* [sequences] */
   const int32_t* page_table;  /* [sequences][table_width] */
   int32_t max_new;            /* upper bounds of the sequences' new tokens */
-  int32_t max_cached;         /* and of their cached ones */
+  int32_t max_cached;         /* and of their cached ones: attention is laid out
+                                 for it, and a sequence with more is attended
+                                 in full, only slower */
 } lrqat_kv_batch;
 
 /*

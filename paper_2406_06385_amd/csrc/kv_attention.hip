@@ -89,7 +89,7 @@ __device__ __forceinline__ bool tile_of(const KvAttnArgs& a, int rows_per_tile, 
   t.c0 = q.c0;
   t.rows = int(q.end - q.c0) * a.group;
   t.last = int(min(q.end, int64_t(a.b.width) << a.c.lpage) - 1);
-  t.split_up = t.last >= a.chunk;
+  t.split_up = kv_splits(t.last, a.chunk, a.nsplit) > 1;
   return t.r0 < t.rows;
 }
 // The last key that row r of the tile's sequence sees; -1 past its rows.
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(64 * NW, DH == 4 ? 1 : 2) void k_kv_attn_rows(KvAtt
   const uint32_t qi = uint32_t(rr) / uint32_t(a.group), head = tl.head * a.group + uint32_t(rr) % uint32_t(a.group);
   const int64_t token = tl.row0 + qi;
   const int limit = row_limit(a, tl, rr);
-  const int k0 = tl.split * a.chunk, k1 = kv_split_end(tl.split, a.chunk, row_limit(a, tl, min(tl.r0 + kRowTile, tl.rows) - 1) + 1);
+  const int k0 = tl.split * a.chunk, k1 = kv_split_end(tl.split, a.nsplit, a.chunk, row_limit(a, tl, min(tl.r0 + kRowTile, tl.rows) - 1) + 1);
   if (k0 >= k1 && tl.split > 0) return;  // (split 0 of a sequence without keys writes its zeros)
 
   u32x4 qf[DH][2];
@@ -371,7 +371,7 @@ __global__ __launch_bounds__(64 * NW, DP == 256 ? 1 : 2) void k_kv_attn_many(KvA
   const int64_t token = tl.row0 + qi;
   const int limit = row_limit(a, tl, rr);
   const int wave_first = row_limit(a, tl, w0), wave_last = row_limit(a, tl, min(w0 + 31, max(tl.rows - 1, w0)));
-  const int k0 = tl.split * a.chunk, k1 = kv_split_end(tl.split, a.chunk, row_limit(a, tl, min(tl.r0 + 32 * NW, tl.rows) - 1) + 1);
+  const int k0 = tl.split * a.chunk, k1 = kv_split_end(tl.split, a.nsplit, a.chunk, row_limit(a, tl, min(tl.r0 + 32 * NW, tl.rows) - 1) + 1);
   if (k0 >= k1 && tl.split > 0) return;
 
   u32x4 qf[DP / 16];
@@ -625,10 +625,10 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(KvAttnArgs a, uint32_t tas
   const KvSeq q = kv_seq(a.b, seq);
   if (qi >= q.end - q.c0) return;
   const int64_t last = min(q.end, int64_t(a.b.width) << a.c.lpage) - 1;
-  if (last < a.chunk) return;  // one split: written already
+  if (kv_splits(last, a.chunk, a.nsplit) == 1) return;  // written already
   const int64_t token = q.row0 + qi;
   const int64_t limit = a.causal ? min(q.c0 + qi, last) : last;
-  const int ns = int(min(limit / a.chunk + 1, int64_t(a.nsplit)));
+  const int ns = kv_splits(limit, a.chunk, a.nsplit);
   const int64_t step = a.b.tokens * a.hq, at0 = token * a.hq + head;
   const bool in = col < d;
   // the common maximum (every wave or thread for itself); then the splits' outputs in that scale

@@ -74,10 +74,15 @@ inline KvAttnPlan kv_attn_plan(const KvSizes& z) {
   return p;
 }
 
-// The keys of a split among the first `seen`: from split * chunk up to here (at or below that: none).  The sum is formed
-// only where it is a key, as the splits of 2^31 - 2^16 positions may end past 2^31.
-constexpr int kv_split_end(int split, int chunk, int seen) {
-  return seen - split * chunk > chunk ? split * chunk + chunk : seen;
+// The keys of a split among the first `seen`: from split * chunk up to here (at or below that: none).  The last split
+// has all that follow: the lengths are device memory, and a sequence longer than the plan was made for costs time but
+// needs no split, and no partial results, that the workspace does not have.  Within the plan the sum stays below 2^31.
+constexpr int kv_split_end(int split, int nsplit, int chunk, int seen) {
+  return split + 1 < nsplit && (split + 1) * chunk < seen ? (split + 1) * chunk : seen;
+}
+// Splits that the keys 0 .. last fall into (1 where there are none): more than one are joined from partial results.
+constexpr int kv_splits(int64_t last, int chunk, int nsplit) {
+  return last / chunk + 1 < nsplit ? int(last / chunk) + 1 : nsplit;
 }
 
 }  // namespace lrqat

@@ -1,5 +1,5 @@
 // Host driver for the splits of attention over the KV cache: reads lines "heads d hq seqs max_new max_cached tokens
-// capacity seen" and prints "chunk nsplit", then the first key and the end of each split for a row that sees that many.
+// capacity seen" and prints "chunk nsplit splits", then the first key and the end of each split for a row that sees that many.
 #include <cstdio>
 
 #include "kv_plan.h"
@@ -14,8 +14,8 @@ int main() {
     z.tokens = tokens;
     z.capacity = capacity;
     const KvAttnPlan p = kv_attn_plan(z);
-    std::printf("%d %d", p.chunk, p.nsplit);
-    for (int s = 0; s < p.nsplit; ++s) std::printf(" %d %d", s * p.chunk, kv_split_end(s, p.chunk, seen));
+    std::printf("%d %d %d", p.chunk, p.nsplit, kv_splits(int64_t(seen) - 1, p.chunk, p.nsplit));
+    for (int s = 0; s < p.nsplit; ++s) std::printf(" %d %d", s * p.chunk, kv_split_end(s, p.nsplit, p.chunk, seen));
     std::printf("\n");
   }
   return 0;

@@ -20,6 +20,9 @@ def lr():
     return lrqat
 
 
+from test_gpu_kv_attention import Setup
+
+
 def _dev(a):
     return torch.from_numpy(np.ascontiguousarray(np.asarray(a, np.int32))).cuda()
 
@@ -43,3 +46,33 @@ def test_the_last_positions_of_a_full_table(lr):
     k, v = (t[[2, 0, 1], 0].double().reshape(-1, d) * 0.01 for t in (cache.k, cache.v))
     p = torch.softmax(k @ q[0, 0].double() * d ** -0.5, 0)
     assert ((O[0, 0].double() - p @ v).abs() <= 2.0 ** -8 * (p @ v).abs() + 2.0 ** -10 * (p @ v.abs())).all()
+
+
+# hq, hkv, d, page, block, new, cached, and the bound that the batch gives in place of the largest cached
+OVER = {
+    "one token, no splits": (32, 8, 128, 64, 1, [1], [700], 300),
+    "one token, one key more": (32, 8, 128, 64, 1, [1, 1], [512, 3], 511),
+    "one token, splits": (8, 2, 64, 64, 16, [1, 1], [9000, 40], 3000),
+    "one token, nothing planned": (4, 4, 80, 16, 1, [1, 1, 1], [5000, 0, 700], 0),
+    "128 rows, no splits": (8, 8, 80, 16, 1, [33] * 40, [5] * 20 + [900] * 20, 5),
+    "128 rows, splits": (32, 8, 112, 64, 1, [450], [2000], 400),
+    "256 rows, splits": (32, 8, 128, 64, 16, [300, 7], [6000, 20], 2750),
+}
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("name", list(OVER))
+def test_sequences_longer_than_planned(lr, name, causal):
+    """max_cached below what the device holds: attended in full, and nothing is written past the workspace."""
+    *shape, bound = OVER[name]
+    S = Setup(lr, *shape, seed=62)
+    plain = S.batch()
+    S.batch = lambda: lr.KVBatch(plain.first, plain.cached, plain.page_table, S.tokens, max(S.new), bound)
+    need = lr.lrqat_kv_attention_workspace_size(S.cache, S.batch(), S.hq)
+    assert (need > 256) == ("no" not in name and "one key" not in name)
+    room = torch.full((need + (64 << 20),), 0x5a, dtype=torch.uint8, device="cuda")     # a canary behind the workspace
+    O = S.run(causal, ws=room[:need])
+    torch.cuda.synchronize()
+    assert (room[need:] == 0x5a).all()
+    ref, err = S.reference(causal)
+    assert ((O.double() - ref).abs() <= err).all()
