@@ -65,6 +65,13 @@ __device__ __forceinline__ float below(float mx) {
   return mx - m <= kBias + 1.f ? m : mx;  // (mx where it is an infinity)
 }
 
+// Denominators are held in units of 2^16: a key of a block of zeros adds 2^14 / 2^-100 or twice that, of which float32
+// would hold 2^13; as it is, 2^29, and what the largest scales of bfloat16 values add, 2^14 / 2^121, stays normal too.
+// A lane's terms of a step are added up before they are taken to that unit.
+constexpr float kDen = 0x1p-16f;
+// 1 / l; 0 where no key was seen, NaN where a NaN was.
+__device__ __forceinline__ float reciprocal(float l) { return l > 0.f ? kDen / l : l == l ? 0.f : l; }
+
 // What a block works on.
 struct Tile {
   int seq, head, split;
@@ -224,13 +231,15 @@ __global__ __launch_bounds__(64 * NW, DH == 4 ? 1 : 2) void k_kv_attn_rows(KvAtt
     const float alpha = exp2_(m - mf);
     m = m1;
     l *= alpha;
+    float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < VB; ++e) o[e] *= alpha;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       w[j] = exp2_(w[j] - mf);
-      l = __builtin_fmaf(w[j], rb[TOK ? j : 0], l);
+      sum = __builtin_fmaf(w[j], rb[TOK ? j : 0], sum);
     }
+    l = __builtin_fmaf(sum, kDen, l);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       u32x4 p;
@@ -296,7 +305,7 @@ __global__ __launch_bounds__(64 * NW, DH == 4 ? 1 : 2) void k_kv_attn_rows(KvAtt
   if (wave > 0 || !valid) return;
   // element v of o[e]: column VB (4 g + v) + e
   if (!tl.split_up) {
-    const float r = l > 0.f ? 1.f / l : l == l ? 0.f : l;
+    const float r = reciprocal(l);
     uint16_t* dst = a.o + token * a.o_stride + int64_t(head) * d + 4 * VB * g;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
@@ -533,6 +542,7 @@ __global__ __launch_bounds__(64 * NW, DP == 256 ? 1 : 2) void k_kv_attn_many(KvA
       for (int e = 0; e < DP / 32; ++e) o[e] *= alpha;
     }
     const float mf = m == kNone ? 0.f : m;
+    float sum = 0.f;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -542,7 +552,7 @@ __global__ __launch_bounds__(64 * NW, DP == 256 ? 1 : 2) void k_kv_attn_many(KvA
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           w[j] = exp2_(s[t][8 * u + j] - mf);
-          l = __builtin_fmaf(w[j], r[TOK ? j : 0], l);
+          sum = __builtin_fmaf(w[j], r[TOK ? j : 0], sum);
         }
         u32x4 p;
 #pragma unroll
@@ -550,6 +560,7 @@ __global__ __launch_bounds__(64 * NW, DP == 256 ? 1 : 2) void k_kv_attn_many(KvA
 #pragma unroll
         for (int e = 0; e < DP / 32; ++e) o[e] = mfma32_f16(lds.v[buf][32 * e + c32][4 * t + 2 * u + hh], p, o[e]);
       }
+    l = __builtin_fmaf(sum, kDen, l);
   };
 
   if (steps > 0) {
@@ -574,7 +585,7 @@ __global__ __launch_bounds__(64 * NW, DP == 256 ? 1 : 2) void k_kv_attn_many(KvA
   if (!valid) return;
   // element 4 v + i of o[e]: column (DP / 32) (8 v + 4 hh + i) + e
   constexpr int CE = DP / 32;
-  const float r = l > 0.f ? 1.f / l : l == l ? 0.f : l;
+  const float r = reciprocal(l);
   const int64_t at = (int64_t(tl.split) * a.b.tokens + token) * a.hq + head;
   uint16_t* out = a.o + token * a.o_stride + int64_t(head) * d;
 #pragma unroll
@@ -663,7 +674,7 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(KvAttnArgs a, uint32_t tas
       acc += red_o[i][lane];
     }
   }
-  const float r = l > 0.f ? 1.f / l : l == l ? 0.f : l;
+  const float r = reciprocal(l);
   *reinterpret_cast<u32x2*>(a.o + token * a.o_stride + int64_t(head) * d + col) =
       u32x2{pack_bf16x2(result(acc[0] * r), result(acc[1] * r)), pack_bf16x2(result(acc[2] * r), result(acc[3] * r))};
 }

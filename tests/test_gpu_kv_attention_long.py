@@ -76,3 +76,41 @@ def test_sequences_longer_than_planned(lr, name, causal):
     assert (room[need:] == 0x5a).all()
     ref, err = S.reference(causal)
     assert ((O.double() - ref).abs() <= err).all()
+
+
+@pytest.mark.parametrize("block", [1, 16])
+@pytest.mark.parametrize("hq,hkv,seqs,new", [(8, 8, 64, 1), (64, 4, 1, 1040)], ids=["one token", "256 rows"])
+def test_many_keys_whose_values_are_zeros(lr, hq, hkv, seqs, new, block):
+    """512000 keys with values of zeros (scales of 2^-100, as a write leaves them) ahead of ordinary ones, in one split:
+    they count in the denominator, whose float32 sum in a lane would be 2^15 times 2^114 with one token a sequence and
+    more with many.  One page holds all of the zeros, and one key."""
+    d, page, zeros, own = 16, 64, 8000, 2 + -(-new // 64)
+    cache = lr.lrqat_kv_cache(lr.KVCacheSpec(hkv, d, own + 1, page, block))
+    g = torch.Generator(device="cuda").manual_seed(63)
+    for t in (cache.k, cache.v):
+        t.copy_(torch.randint(-127, 128, t.shape, device="cuda", generator=g, dtype=torch.int8))
+    for t in (cache.k_scale, cache.v_scale):
+        t.fill_(0.01)
+    lr.lrqat_kv_write(cache, lr.KVBatch(_dev([0, page]), _dev([0]), _dev([[0]]), page, page, 0),
+                      torch.randn((1, hkv, d), device="cuda", generator=g).repeat(page, 1, 1), torch.zeros((page, hkv, d), device="cuda"))
+    assert (cache.v_scale[0] == 2.0 ** -100).all()
+    total = (zeros + own) * page - 5
+    row = [0] * zeros + list(range(1, own + 1))
+    batch = lr.KVBatch(_dev(np.arange(seqs + 1) * new), _dev([total - new] * seqs), _dev([row] * seqs), seqs * new, new,
+                       total - new)
+    q = torch.randn((seqs * new, hq, d), device="cuda", generator=g).to(torch.bfloat16)
+    assert lr.lrqat_kv_attention_workspace_size(cache, batch, hq) == 256
+    O = lr.lrqat_kv_attention(cache, batch, q)
+    pages = torch.tensor(row, device="cuda")
+    rows = torch.arange(0, seqs * new, 13, device="cuda")
+    last = total - new + rows % new
+    for h in range(0, hq, 3):
+        k, v = (c[pages, h * hkv // hq].double().reshape(-1, d)[:total]
+                * s[pages, h * hkv // hq].double().repeat_interleave(block, 1).reshape(-1, 1)[:total]
+                for c, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)))
+        z = q[rows, h].double() @ k.t().contiguous() * d ** -0.5
+        p = torch.softmax(z.masked_fill(torch.arange(total, device="cuda") > last[:, None], -math.inf), 1)
+        # the smallest weights, as in test_gpu_kv_attention: 2^-39 of the largest p b, on codes of at most 127
+        err = 2.0 ** -8 * (p @ v).abs() + 2.0 ** -10 * (p @ v.abs()) + 2.0 ** -39 * 127 * own * page * 0.01 * p.amax(1, keepdim=True)
+        assert ((O[rows, h].double() - p @ v).abs() <= err).all()
+        assert (O[rows, h] != 0).any()

@@ -179,3 +179,10 @@ def test_strides_and_in_place(lr, key):
     assert torch.equal(wide[:, 2:S.hq + 2], ref) and (wide[:, :2] == 7).all() and (wide[:, S.hq + 2] == 7).all()
     lr.lrqat_kv_attention(S.cache, S.batch(), dense, scale=S.scale, O=dense)
     assert torch.equal(dense, ref)
+
+
+@pytest.mark.parametrize("key", list(FEW) + SOME, ids=list(FEW) + SOME_IDS)
+def test_values_near_the_end_of_bfloat16(lr, key):
+    S = Setup(lr, *(FEW[key] if key in FEW else SHAPES[key]), seed=60)
+    S.cache.v_scale *= 2.0 ** 115
+    S.check()
