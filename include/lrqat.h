@@ -276,8 +276,9 @@ lrqat_status lrqat_infer_forward_codes(const lrqat_layer* layer, int64_t tokens,
  *         written as 0); n_sum is nullable by itself
  * At least one output is wanted.  y is computed from the float32 h, not from
  * the rounded one, and its codes from the float32 y.  A token with a NaN or an
- * infinity gets s_x = NaN, a token of zeros s_x = 0.  width <= 65536
- * (LRQAT_EUNSUPPORTED beyond).  T = 0 is a no-op.
+ * infinity (in h or in gain h, or as the sum of its squares) gets s_x = NaN, a
+ * token of zeros s_x = 0.  width <= 65536 (LRQAT_EUNSUPPORTED beyond).  T = 0
+ * is a no-op.
  */
 lrqat_status lrqat_rmsnorm_forward(int64_t tokens, int64_t width, int32_t act_dtype, const void* X,
                                    const void* R, const float* gain, float eps, void* H, void* Y,

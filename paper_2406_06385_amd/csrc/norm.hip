@@ -72,14 +72,17 @@ __device__ __forceinline__ void store8(float* p, int64_t valid, const float* f) 
   }
 }
 
-// Wave totals of a (and of b: a sum, or a maximum), then of the row's waves, in a fixed order.
+// The larger of two magnitudes, or a NaN where either is one: as integers, NaN lies above infinity and that above numbers.
+__device__ __forceinline__ float larger(float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }
+
+// Wave totals of a (and of b: a sum, or the largest of magnitudes), then of the row's waves, in a fixed order.
 template <bool ONE, bool MAX>
 __device__ __forceinline__ void row_reduce(float& a, float& b, float (*red)[2]) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) {
     a += __shfl_xor(a, off);
     const float o = __shfl_xor(b, off);
-    b = MAX ? fmaxf(b, o) : b + o;
+    b = MAX ? larger(b, o) : b + o;
   }
   if constexpr (!ONE) {
     const int w = int(threadIdx.x >> 6), nw = int(blockDim.x >> 6);
@@ -92,7 +95,7 @@ __device__ __forceinline__ void row_reduce(float& a, float& b, float (*red)[2]) 
     b = red[0][1];
     for (int i = 1; i < nw; ++i) {
       a += red[i][0];
-      b = MAX ? fmaxf(b, red[i][1]) : b + red[i][1];
+      b = MAX ? larger(b, red[i][1]) : b + red[i][1];
     }
   }
 }
@@ -131,7 +134,7 @@ __global__ __launch_bounds__(1024) void k_rmsnorm(NormArgs a) {
       for (int e = 0; e < 8; ++e) {
         ss = __builtin_fmaf(h[e], h[e], ss);
         hg[i][e] = h[e] * g[e];
-        mx = fmaxf(mx, fabsf(hg[i][e]));
+        mx = larger(mx, fabsf(hg[i][e]));
       }
     }
   }
@@ -179,7 +182,8 @@ __global__ __launch_bounds__(1024) void k_rmsnorm(NormArgs a) {
     }
     if (threadIdx.x == 0) a.nsum[row] = total;
   }
-  if (threadIdx.x == 0) a.sx[row] = rho * mx / 127.f;  // NaN where the row holds a NaN or an infinity
+  // NaN where the row holds a NaN or an infinity, also one that a gain of 0 hides from mx: the row would read as zeros
+  if (threadIdx.x == 0) a.sx[row] = larger(ss, mx) < __builtin_inff() ? rho * mx / 127.f : __builtin_nanf("");
 }
 
 // Eight values as they are loaded.
