@@ -153,7 +153,8 @@ __global__ __launch_bounds__(1024) void k_rmsnorm(NormArgs a) {
     }
   }
   if (!a.codes) return;
-  const float inv = mx > 0.f ? 127.f / mx : 0.f;
+  // 127 / mx would pass float32 from mx < 2^-121 on, and 0 times it be no 0: such rows are lifted by 2^64 first
+  const float lift = mx < 0x1p-100f ? 0x1p64f : 1.f, inv = mx > 0.f ? 127.f / (mx * lift) : 0.f;
   int total = 0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(1024) void k_rmsnorm(NormArgs a) {
       for (int q = 0; q < 2; ++q) {
         uint32_t c[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c[e] = uint32_t(int(__builtin_rintf(__builtin_amdgcn_fmed3f(hg[i][4 * q + e] * inv, -127.f, 127.f))));
+        for (int e = 0; e < 4; ++e) c[e] = uint32_t(int(__builtin_rintf(__builtin_amdgcn_fmed3f(hg[i][4 * q + e] * lift * inv, -127.f, 127.f))));
         total += int(c[0]) + int(c[1]) + int(c[2]) + int(c[3]);
         o[q] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[3], c[2], 0x0c0c0400u), __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400u), 0x05040100u);
       }

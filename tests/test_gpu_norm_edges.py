@@ -63,3 +63,27 @@ def test_squares_past_float32(lr, n):
     x[1, 0] = 1e25
     x[2, n - 1] = -3e38
     assert _codes(lr, x, g).sx.isnan().tolist() == [False, True, True, False]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n", WIDTHS)
+def test_rows_of_the_smallest_values(lr, n, dtype):
+    """Down to subnormal values: with the squares beside eps, y is h g / sqrt(eps), and its codes are those of h g.
+    Powers of 2 times whole numbers, so that h g and its quotients are exact; the scale of the smallest rows is itself
+    subnormal, its last place 2^-149."""
+    whole = torch.randint(-100, 101, (7, n), device="cuda", generator=torch.Generator(device="cuda").manual_seed(74))
+    whole[:, 0] = 100
+    whole[6, 1:] = 0
+    exponents = torch.tensor([-90, -110, -118, -121, -126, -132, -126], device="cuda")
+    x = (whole.double() * torch.exp2(exponents.double())[:, None]).to(dtype)
+    assert torch.equal(x.double(), whole.double() * torch.exp2(exponents.double())[:, None])
+    g = torch.ones(n, device="cuda")
+    q = _codes(lr, x, g)
+    u = whole.double() * 127 / 100
+    assert not (((u - torch.floor(u)) - 0.5).abs() < 1e-4)[whole.abs() != 50].any()
+    off = (q.codes[:, :n].double() - torch.round(u)).abs()
+    assert not off[whole.abs() != 50].any() and off.max() <= 1         # 63.5: either side
+    assert not q.codes[:, n:].any()
+    assert torch.equal(q.nsum, q.codes.sum(1, dtype=torch.int32))
+    s = 100 * torch.exp2(exponents.double()) / EPS ** 0.5 / 127
+    assert ((q.sx.double() - s).abs() <= 2e-6 * s + 2.0 ** -148).all()
