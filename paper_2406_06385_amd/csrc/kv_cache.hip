@@ -79,7 +79,7 @@ __device__ __forceinline__ Place place_of(uint32_t w, uint32_t heads, uint32_t s
 // Codes rint(x / s), the quotient rounded to float32 first; |x / s| <= 127.  Adding 1.5 2^23 rounds to the nearest
 // integer, ties to even, and leaves it in the low bits.  y = x (1 / s) is within 2e-5 of the quotient, so only where y
 // is that near to a rounding point the quotient itself decides (one wave in ten; the quotients of all values took half
-// of the kernel's time).  s = NaN: codes 0.  Lanes that are not live get anything.
+// of the kernel's time).  s = NaN: codes 0, by the same way.  Lanes that are not live get anything.
 constexpr float kRound = 12582912.f;
 __device__ __forceinline__ u32x2 codes_of(const float* x, float s, bool live) {
   const float inv = s == s ? 1.f / s : 0.f;
@@ -91,9 +91,9 @@ __device__ __forceinline__ u32x2 codes_of(const float* x, float s, bool live) {
     c[e] = __float_as_uint(t);
     off = fmaxf(off, fabsf(y - (t - kRound)));
   }
-  if (__any(live && !(off < 0.4999f)))
+  if (__any(live && !(off < 0.4999f && s == s)))
 #pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = __float_as_uint((s == s ? x[e] / s : 0.f) + kRound);
+    for (int e = 0; e < 8; ++e) c[e] = s == s ? __float_as_uint(x[e] / s + kRound) : 0u;  // (0 times a NaN keeps its low bits)
   return low_bytes(c);
 }
 
