@@ -333,7 +333,9 @@ typedef struct {
  * kernels check what they read: rows outside [0, tokens), positions past the
  * table and page numbers outside [0, pages) hold nothing (they are not
  * written, read as 0, and are not attended), and rows of a sequence past
- * max_new are left out.
+ * max_new are left out.  A sequence that ends past `tokens` is cut there; one
+ * that starts at a negative row or position has no rows.  Rows of the outputs
+ * that no sequence has are left as they are.
  */
 typedef struct {
   int32_t sequences;          /* 0 .. 65535 */

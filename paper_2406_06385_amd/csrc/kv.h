@@ -37,11 +37,11 @@ struct KvSeq {
 
 // Sequence s of the batch, cut to the batch's rows; c0 = end where it has none.
 __device__ __forceinline__ KvSeq kv_seq(const KvBatch& b, int s) {
-  const int64_t f0 = b.first[s], f1 = b.first[s + 1];
+  const int64_t f0 = b.first[s], f1 = min(int64_t(b.first[s + 1]), b.tokens);
   KvSeq q;
   q.row0 = f0;
   q.c0 = b.cached[s];
-  const bool ok = f0 >= 0 && f1 <= b.tokens && f1 > f0 && q.c0 >= 0;
+  const bool ok = f0 >= 0 && f1 > f0 && q.c0 >= 0;
   q.end = ok ? q.c0 + min(f1 - f0, int64_t(b.max_new)) : q.c0;
   return q;
 }
