@@ -822,7 +822,7 @@ static lrqat_status kv_io(const lrqat_kv_cache* cache, const lrqat_kv_batch* bat
   LRQAT_TRY(kv_pointers(cache, batch));
   LRQAT_TRY(kv_rows("K", K, k_stride, int64_t(c.heads) * c.d, b.tokens, act_dtype));
   LRQAT_TRY(kv_rows("V", V, v_stride, int64_t(c.heads) * c.d, b.tokens, act_dtype));
-  if (kv_units(c, b, write) >= INT32_MAX)
+  if (!kv_fits(c, b, write))
     return fail(LRQAT_EUNSUPPORTED, "%d sequences of up to %d tokens with %d heads are more than one launch holds", b.seqs,
                 b.max_new, c.heads);
   return LRQAT_OK;
@@ -856,7 +856,7 @@ static lrqat_status kv_attn_args(const lrqat_kv_cache* cache, const lrqat_kv_bat
   if (q_heads < 1 || q_heads > 65536 || q_heads % c.heads)
     return fail(LRQAT_EINVAL, "q_heads must be a multiple of kv_heads up to 65536 (got %d and %d)", q_heads, c.heads);
   p = kv_attn_plan(KvSizes{c.heads, c.d, q_heads, b.seqs, b.max_new, b.max_cached, b.tokens, int64_t(b.width) << c.lpage});
-  if (p.blocks >= INT32_MAX || int64_t(b.seqs) * b.max_new * q_heads >= INT32_MAX / 8)  // (8 blocks join a row)
+  if (!kv_attention_fits(c, b, q_heads, p))
     return fail(LRQAT_EUNSUPPORTED, "%d sequences of up to %d tokens with %d heads are more than one launch holds", b.seqs,
                 b.max_new, q_heads);
   return LRQAT_OK;

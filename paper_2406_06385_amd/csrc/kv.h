@@ -10,6 +10,8 @@ namespace lrqat {
 // below kKvMinScale, so that a block of zeros needs no case of its own anywhere.
 constexpr float kKvMinScale = 0x1p-100f;
 
+constexpr int64_t kMaxThreads = int64_t(UINT32_MAX);  // of a grid
+
 struct KvCache {
   int8_t* code[2];   // K, V
   float* scale[2];
@@ -81,8 +83,8 @@ struct KvReadArgs {
   void* x[2];
   int64_t stride[2];
 };
-// units of work of a launch (the host checks that the grid holds them)
-int64_t kv_units(const KvCache& c, const KvBatch& b, bool write);
+// Whether one launch holds the batch (the host checks).
+bool kv_fits(const KvCache& c, const KvBatch& b, bool write);
 hipError_t launch_kv_write(bool bf16, const KvWriteArgs& a, hipStream_t st);
 hipError_t launch_kv_read(bool bf16, const KvReadArgs& a, hipStream_t st);
 
@@ -102,6 +104,7 @@ struct KvAttnArgs {
   float* part_o;       // [nsplit][tokens][hq][d] where nsplit > 1
   float* part_ml;      // [nsplit][tokens][hq][2]: maximum of the weights' exponents, denominator
 };
+bool kv_attention_fits(const KvCache& c, const KvBatch& b, int hq, const KvAttnPlan& p);
 hipError_t launch_kv_attention(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t st);
 
 }  // namespace lrqat

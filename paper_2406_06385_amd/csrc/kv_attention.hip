@@ -691,7 +691,18 @@ void launch_many(const KvAttnArgs& a, unsigned blocks, hipStream_t st) {
   else k_kv_attn_many<DP, false, NW><<<blocks, 64 * NW, sizeof(ManyLds<DP, false>), st>>>(a);
 }
 
+bool wide_join(int64_t tasks, int nsplit) { return nsplit > 4 && tasks < 2048; }
+int64_t join_blocks(int64_t tasks, int d, int nsplit) {
+  return wide_join(tasks, nsplit) ? tasks * ((d + 31) / 32) : (tasks + 256 / (d / 4) - 1) / (256 / (d / 4));
+}
+
 }  // namespace
+
+bool kv_attention_fits(const KvCache& c, const KvBatch& b, int hq, const KvAttnPlan& p) {
+  const int64_t tasks = int64_t(b.seqs) * b.max_new * hq;  // (rows of tiles and of the join are counted in 32 bits)
+  return tasks < INT32_MAX / 8 && p.blocks <= kMaxThreads / (64 * p.waves) &&
+         (p.nsplit == 1 || join_blocks(tasks, c.d, p.nsplit) <= kMaxThreads / 256);
+}
 
 hipError_t launch_kv_attention(const KvAttnArgs& a, const KvAttnPlan& p, hipStream_t st) {
   const unsigned blocks = unsigned(p.blocks);
@@ -707,8 +718,9 @@ hipError_t launch_kv_attention(const KvAttnArgs& a, const KvAttnPlan& p, hipStre
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
   const int64_t tasks = int64_t(a.b.seqs) * a.b.max_new * a.hq;
-  if (p.nsplit > 4 && tasks < 2048) k_kv_attn_join<32><<<unsigned(tasks * ((d + 31) / 32)), 256, 0, st>>>(a, uint32_t(tasks));
-  else k_kv_attn_join<1><<<unsigned((tasks + 256 / (d / 4) - 1) / (256 / (d / 4))), 256, 0, st>>>(a, uint32_t(tasks));
+  const unsigned joins = unsigned(join_blocks(tasks, d, p.nsplit));
+  if (wide_join(tasks, p.nsplit)) k_kv_attn_join<32><<<joins, 256, 0, st>>>(a, uint32_t(tasks));
+  else k_kv_attn_join<1><<<joins, 256, 0, st>>>(a, uint32_t(tasks));
   return hipGetLastError();
 }
 

@@ -287,17 +287,26 @@ int64_t spans_of(const KvCache& c, const KvBatch& b, bool write) {
   return write ? ((int64_t(b.max_new) - 2 + (int64_t(1) << l)) >> l) + 1 : (int64_t(b.max_new) - 1 + (int64_t(1) << l)) >> l;
 }
 
-}  // namespace
-
-int64_t kv_units(const KvCache& c, const KvBatch& b, bool write) {
+int64_t units_of(const KvCache& c, const KvBatch& b, bool write) {
   return int64_t(b.seqs) * spans_of(c, b, write) * 2 * c.heads;
 }
 
+WriteMode write_mode(const KvCache& c) {
+  const int own = 6 - lanes_log2(c.d) + 2;  // log2 of a wave's tokens
+  return c.lscale > own ? kShared : own <= c.lpage ? kOnePage : kPages;
+}
+
+}  // namespace
+
+bool kv_fits(const KvCache& c, const KvBatch& b, bool write) {
+  const int64_t units = units_of(c, b, write);
+  return (write && write_mode(c) == kShared ? units : (units + kWaves - 1) / kWaves) <= kMaxThreads / (64 * kWaves);
+}
+
 hipError_t launch_kv_write(bool bf16, const KvWriteArgs& a, hipStream_t st) {
-  const uint32_t units = uint32_t(kv_units(a.c, a.b, true)), spans = uint32_t(spans_of(a.c, a.b, true));
+  const uint32_t units = uint32_t(units_of(a.c, a.b, true)), spans = uint32_t(spans_of(a.c, a.b, true));
   const int lg = lanes_log2(a.c.d);
-  const int own = 6 - lg + 2;  // log2 of a wave's tokens
-  const int mode = a.c.lscale > own ? kShared : own <= a.c.lpage ? kOnePage : kPages;
+  const WriteMode mode = write_mode(a.c);
   const dim3 grid(mode == kShared ? units : (units + kWaves - 1) / kWaves), block(64, kWaves);
   const auto run = [&](auto type) {
     using T = decltype(type);
@@ -311,7 +320,7 @@ hipError_t launch_kv_write(bool bf16, const KvWriteArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_kv_read(bool bf16, const KvReadArgs& a, hipStream_t st) {
-  const uint32_t units = uint32_t(kv_units(a.c, a.b, false)), spans = uint32_t(spans_of(a.c, a.b, false));
+  const uint32_t units = uint32_t(units_of(a.c, a.b, false)), spans = uint32_t(spans_of(a.c, a.b, false));
   const dim3 grid((units + kWaves - 1) / kWaves), block(64, kWaves);
   if (bf16) k_kv_read<uint16_t><<<grid, block, 0, st>>>(a, lanes_log2(a.c.d), spans, units);
   else k_kv_read<float><<<grid, block, 0, st>>>(a, lanes_log2(a.c.d), spans, units);
