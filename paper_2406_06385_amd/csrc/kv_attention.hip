@@ -96,7 +96,7 @@ __device__ __forceinline__ bool tile_of(const KvAttnArgs& a, int rows_per_tile, 
   t.c0 = q.c0;
   t.rows = int(q.end - q.c0) * a.group;
   t.last = int(min(q.end, int64_t(a.b.width) << a.c.lpage) - 1);
-  t.split_up = kv_splits(t.last, a.chunk, a.nsplit) > 1;
+  t.split_up = kv_split_up(t.last, a.chunk, a.nsplit);
   return t.r0 < t.rows;
 }
 // The last key that row r of the tile's sequence sees; -1 past its rows.
@@ -636,7 +636,7 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(KvAttnArgs a, uint32_t tas
   const KvSeq q = kv_seq(a.b, seq);
   if (qi >= q.end - q.c0) return;
   const int64_t last = min(q.end, int64_t(a.b.width) << a.c.lpage) - 1;
-  if (kv_splits(last, a.chunk, a.nsplit) == 1) return;  // written already
+  if (!kv_split_up(last, a.chunk, a.nsplit)) return;  // written already
   const int64_t token = q.row0 + qi;
   const int64_t limit = a.causal ? min(q.c0 + qi, last) : last;
   const int ns = kv_splits(limit, a.chunk, a.nsplit);

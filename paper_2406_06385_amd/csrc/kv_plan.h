@@ -80,7 +80,9 @@ inline KvAttnPlan kv_attn_plan(const KvSizes& z) {
 constexpr int kv_split_end(int split, int nsplit, int chunk, int seen) {
   return split + 1 < nsplit && (split + 1) * chunk < seen ? (split + 1) * chunk : seen;
 }
-// Splits that the keys 0 .. last fall into (1 where there are none): more than one are joined from partial results.
+// Whether the keys 0 .. last fall into more than one split, which are joined from partial results; and into how many (1
+// where there are none).
+constexpr bool kv_split_up(int64_t last, int chunk, int nsplit) { return nsplit > 1 && last >= chunk; }
 constexpr int kv_splits(int64_t last, int chunk, int nsplit) {
   return last / chunk + 1 < nsplit ? int(last / chunk) + 1 : nsplit;
 }

@@ -14,7 +14,9 @@ int main() {
     z.tokens = tokens;
     z.capacity = capacity;
     const KvAttnPlan p = kv_attn_plan(z);
-    std::printf("%d %d %d", p.chunk, p.nsplit, kv_splits(int64_t(seen) - 1, p.chunk, p.nsplit));
+    const int count = kv_splits(int64_t(seen) - 1, p.chunk, p.nsplit);
+    if (kv_split_up(int64_t(seen) - 1, p.chunk, p.nsplit) != (count > 1)) return 1;
+    std::printf("%d %d %d", p.chunk, p.nsplit, count);
     for (int s = 0; s < p.nsplit; ++s) std::printf(" %d %d", s * p.chunk, kv_split_end(s, p.nsplit, p.chunk, seen));
     std::printf("\n");
   }
