@@ -203,15 +203,17 @@ def _checked_ptr(t):
     return t.data_ptr()
 
 
-# the current stream's handle without a Stream object around it, where torch offers that
+# the current stream's handle without a Stream object around it, and the current device without a check that the GPU is
+# initialised (calls have tensors on it), where torch offers those
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream):
     if stream is not None:
         return stream.cuda_stream
     if _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(_raw_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -608,16 +610,21 @@ class KVCache(_StructSlot):
         _expect(self.v_scale, sp.scale_shape(), torch.float32, "v_scale", dev)
 
     @property
-    def _c(self):
-        # the tensors are held and the fields frozen, so one struct serves every call
+    def _ref(self):
+        """The C struct's address.  The struct is made once, and again where a tensor's memory has been exchanged since
+        (by set_(), by .data, by a resize_() that moved it): its sizes may have gone with it, so they are checked too."""
+        at = (self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr())
         try:
-            return self._struct
+            ref, was = self._struct
+            if was == at:
+                return ref
         except AttributeError:
-            sp = self.spec
-            object.__setattr__(self, "_struct", _KVCache(
-                sp.kv_heads, sp.head_dim, sp.page_tokens, sp.scale_tokens, sp.pages, self.k.data_ptr(),
-                self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr()))
-            return self._struct
+            pass
+        self.__post_init__()
+        sp = self.spec
+        ref = ctypes.byref(_KVCache(sp.kv_heads, sp.head_dim, sp.page_tokens, sp.scale_tokens, sp.pages, *at))
+        object.__setattr__(self, "_struct", (ref, at))
+        return ref
 
     def __getstate__(self):
         return dict(self.__dict__)
@@ -652,14 +659,20 @@ class KVBatch(_StructSlot):
                 dev)
 
     @property
-    def _c(self):
+    def _ref(self):
+        """As a cache's."""
+        at = (self.first.data_ptr(), self.cached.data_ptr(), self.page_table.data_ptr())
         try:
-            return self._struct
+            ref, was = self._struct
+            if was == at:
+                return ref
         except AttributeError:
-            object.__setattr__(self, "_struct", _KVBatch(
-                self.cached.numel(), self.page_table.shape[1], self.tokens, self.first.data_ptr(),
-                self.cached.data_ptr(), self.page_table.data_ptr(), self.max_new, self.max_cached))
-            return self._struct
+            pass
+        self.__post_init__()
+        ref = ctypes.byref(_KVBatch(self.cached.numel(), self.page_table.shape[1], self.tokens, *at, self.max_new,
+                                    self.max_cached))
+        object.__setattr__(self, "_struct", (ref, at))
+        return ref
 
     def __getstate__(self):
         return dict(self.__dict__)
@@ -670,13 +683,13 @@ def _rows(t, tokens, heads, d, dtypes, name, device):
     distance in elements."""
     if not isinstance(t, _Tensor):
         raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
-    if t.dim() != 3 or t.shape != (tokens, heads, d) or t.dtype not in dtypes:
+    if t.shape != (tokens, heads, d) or t.dtype not in dtypes:
         raise ValueError(f"{name}: expected {(tokens, heads, d)} in {' or '.join(str(x) for x in dtypes)}, got "
                          f"{tuple(t.shape)} {t.dtype}")
     s = t.stride()
-    if t.numel() and (s[2] != 1 or (heads > 1 and s[1] != d)):
+    if (s[2] != 1 or (heads > 1 and s[1] != d)) and t.numel():
         raise ValueError(f"{name}: the heads of a token must be dense (strides {s})")
-    if not t.is_cuda or t.device != device:
+    if t.device != device:  # (the cache's, which is a GPU)
         raise ValueError(f"{name}: on {t.device}, expected {device}")
     return s[0] if tokens > 1 else heads * d
 
@@ -694,7 +707,7 @@ def lrqat_kv_write(cache: KVCache, batch: KVBatch, K, V, stream=None):
     """Quantise the batch's K and V [tokens][kv_heads][head_dim] into the cache.  Tokens may lie any multiple of 16
     bytes apart (columns of a fused projection)."""
     pair = _kv_pair(cache, batch, K, V)
-    _check(_lib().lrqat_kv_write(ctypes.byref(cache._c), ctypes.byref(batch._c), _ACT[K.dtype], *pair,
+    _check(_lib().lrqat_kv_write(cache._ref, batch._ref, _ACT[K.dtype], *pair,
                                  _stream(stream)))
 
 
@@ -708,12 +721,12 @@ def lrqat_kv_read(cache: KVCache, batch: KVBatch, K=None, V=None, dtype=torch.bf
             K = torch.empty(shape, dtype=dt, device=cache.k.device) if K is None else K
             V = torch.empty(shape, dtype=dt, device=cache.k.device) if V is None else V
     pair = _kv_pair(cache, batch, K, V)
-    _check(_lib().lrqat_kv_read(ctypes.byref(cache._c), ctypes.byref(batch._c), _ACT[K.dtype], *pair, _stream(stream)))
+    _check(_lib().lrqat_kv_read(cache._ref, batch._ref, _ACT[K.dtype], *pair, _stream(stream)))
     return K, V
 
 
 def lrqat_kv_attention_workspace_size(cache: KVCache, batch: KVBatch, q_heads: int) -> int:
-    n = _lib().lrqat_kv_attention_workspace_size(ctypes.byref(cache._c), ctypes.byref(batch._c), q_heads)
+    n = _lib().lrqat_kv_attention_workspace_size(cache._ref, batch._ref, q_heads)
     if n == 0:
         raise LRQATError(LRQAT_EINVAL, _lib().lrqat_last_error().decode())
     return n
@@ -735,7 +748,7 @@ def lrqat_kv_attention(cache: KVCache, batch: KVBatch, Q, scale=None, causal=Tru
                 ws = workspace(lrqat_kv_attention_workspace_size(cache, batch, heads), dev)
     os_ = _rows(O, batch.tokens, heads, sp.head_dim, (torch.bfloat16,), "O", dev)
     _expect(ws, (ws.numel(),), torch.uint8, "ws", dev)
-    _check(_lib().lrqat_kv_attention(ctypes.byref(cache._c), ctypes.byref(batch._c), heads, BF16, Q.data_ptr(), qs,
+    _check(_lib().lrqat_kv_attention(cache._ref, batch._ref, heads, BF16, Q.data_ptr(), qs,
                                      sp.head_dim ** -0.5 if scale is None else scale, int(bool(causal)), O.data_ptr(),
                                      os_, ws.data_ptr(), ws.numel(), _stream(stream)))
     return O
