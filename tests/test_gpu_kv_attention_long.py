@@ -114,3 +114,66 @@ def test_many_keys_whose_values_are_zeros(lr, hq, hkv, seqs, new, block):
         err = 2.0 ** -8 * (p @ v).abs() + 2.0 ** -10 * (p @ v.abs()) + 2.0 ** -39 * 127 * own * page * 0.01 * p.amax(1, keepdim=True)
         assert ((O[rows, h].double() - p @ v).abs() <= err).all()
         assert (O[rows, h] != 0).any()
+
+
+def test_a_recorded_step_that_grows_from_one_split_into_the_next(lr):
+    """Write and attention recorded once and replayed as the sequence grows, past the end of the first split and past
+    max_cached: the bits of the calls made one by one, and float64's values."""
+    S = Setup(lr, 8, 2, 64, 64, 16, [1], [1400], seed=64)
+    first, cached, table = _dev([0, 1]), _dev([0]), _dev(S.table)
+    batch = lr.KVBatch(first, cached, table, 1, 1, 1200)
+    need = lr.lrqat_kv_attention_workspace_size(S.cache, batch, S.hq)
+    assert need > 256                                       # split (after 512 keys)
+    ws, out = lr.workspace(need), torch.empty((1, S.hq, S.d), dtype=torch.bfloat16, device="cuda")
+    x = torch.zeros((1, S.hq + 2 * S.hkv, S.d), dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        lr.lrqat_kv_write(S.cache, batch, x[:, S.hq:S.hq + S.hkv], x[:, S.hq + S.hkv:])
+        return lr.lrqat_kv_attention(S.cache, batch, x[:, :S.hq], O=out, ws=ws)
+
+    parts = (S.cache.k, S.cache.v, S.cache.k_scale, S.cache.v_scale)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    g = torch.Generator(device="cuda").manual_seed(65)
+    S.q = x[:, :S.hq]
+    for n in [*range(505, 520), 640, *range(1020, 1028), 1199, 1200, 1201, 1300, 3, 511, 512, 1400]:
+        x.copy_(torch.randn(x.shape, device="cuda", generator=g))
+        cached.fill_(n)
+        before = [t.clone() for t in parts]
+        graph.replay()
+        torch.cuda.synchronize()
+        got, after = out.clone(), [t.clone() for t in parts]
+        for t, b in zip(parts, before):
+            t.copy_(b)
+        ws.fill_(0xff)
+        want = step().clone()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), n
+        assert all(torch.equal(a.view(torch.uint8), t.view(torch.uint8)) for a, t in zip(after, parts))
+        S.cached = [n]
+        ref, err = S.reference(True)
+        assert ((got.double() - ref).abs() <= err).all(), n
+
+
+@pytest.mark.parametrize("shape", [(4, 1, 128, 64, 1, [1], [9000]), (32, 8, 128, 64, 1, [300], [2750])],
+                         ids=["one token", "256 rows"])
+def test_splits_on_a_stream_of_their_own(lr, shape):
+    S = Setup(lr, *shape, seed=66)
+    q = S.q.contiguous()
+    want, batch = lr.lrqat_kv_attention(S.cache, S.batch(), q), S.batch()
+    O = torch.zeros_like(q)
+    ws = lr.workspace(lr.lrqat_kv_attention_workspace_size(S.cache, batch, S.hq)).fill_(0xff)
+    later = torch.zeros_like(q)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        a = torch.randn(2048, 2048, device="cuda")
+        for _ in range(8):                                  # what the call has to wait for
+            a = (a @ a).tanh_()
+        later.copy_(q)
+    lr.lrqat_kv_attention(S.cache, batch, later, O=O, ws=ws, stream=side)   # the current stream is another one
+    side.synchronize()
+    assert torch.equal(O, want)
