@@ -13,7 +13,8 @@
 // scores leave the first product in the lanes that the second one wants them in.  The order of the contracted
 // index is free as long as both operands use the same one: keys are dealt to the rows of the first product so
 // that each lane ends up with 16 consecutive keys, and their values are read a few bytes of 16 rows at a time,
-// which makes the transposition part of the conversion.  Nothing but the join of the waves goes through LDS.
+// which makes the transposition part of the conversion.  With few rows nothing but the join of the waves goes through
+// LDS; with many, the block's waves share what they read there.
 //
 // Rows of the query tokens and of the query heads that share a key/value head are one list: grouped heads read
 // the cache once.  A long axis is split over blocks (whole chunks of keys, so that ragged batches stay even),

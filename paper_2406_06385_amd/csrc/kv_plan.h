@@ -31,8 +31,12 @@ struct KvAttnPlan {
 // the others (32 query and 8 key/value heads of 128): one sequence of 128 new tokens after 400 cached ones 12 and 22,
 // after 1500 22 and 29, after 8000 75 and 56; eight of them after 400 52 and 26; eight of 32 after 1500 32 and 32,
 // after 8000 134 and 74.
-// 256 rows against 128, us: 2000 new tokens 83 and 77, 4000 172 and 189, 8192 646 and 687; 2000 after 2000 cached ones
-// 156 and 158, after 16000 649 and 701.
+// 256 rows against 128, us, medians of 11 runs in turn (the same heads): prompts of 2000 tokens 77 and 70, 2500 96 and 89,
+// 3000 113 and 108, 3500 137 and 149, 4000 170 and 188, 8192 626 and 662; 1000 after 1500 cached ones 72 and 77, after
+// 3000 99 and 107; 2000 after 500 95 and 87, after 1000 113 and 105, after 2000 148 and 140, after 6000 285 and 295,
+// after 16000 626 and 676.  At d = 64: 3000 79 and 76, 4000 116 and 111, 8192 428 and 403; 1000 after 3000 67 and 71; 2000
+// after 2000 103 and 96, after 16000 421 and 453.  So how the blocks fill the chip decides as much as the keys do: the
+// limit of 3000 has the larger gains on its side, and the sizes just above it where 128 rows are 4 to 9% faster.
 inline KvAttnPlan kv_attn_plan(const KvSizes& z) {
   KvAttnPlan p{};
   const int64_t group = z.hq / z.heads, longest = std::max<int64_t>(1, std::min(int64_t(z.max_new) + z.max_cached, z.capacity));

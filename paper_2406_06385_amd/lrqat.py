@@ -641,7 +641,8 @@ def lrqat_kv_cache(spec: KVCacheSpec, device="cuda") -> KVCache:
 class KVBatch(_StructSlot):
     """The tokens of one step: sequence i has rows first[i] .. first[i + 1] - 1 of the step's tensors, at the positions
     that follow its cached[i] earlier tokens; page_table[i] lists the pages of its positions.  One batch serves every
-    layer's calls of a step.  max_new and max_cached bound the sequences' new and cached tokens."""
+    layer's calls of a step.  max_new and max_cached bound the sequences' new and cached tokens: new tokens past max_new are
+    left out; more cached ones than max_cached are attended, only slower."""
     first: torch.Tensor        # int32 [sequences + 1]
     cached: torch.Tensor       # int32 [sequences]
     page_table: torch.Tensor   # int32 [sequences][width]
